@@ -395,6 +395,8 @@ int gc_layer_norm_grads(const void *x, const void *dy, const float *gamma, const
  * entries, in pieces of the vocabulary, so that the logits are never in memory:
  *   z[r][v] = sum_x H[r][x] W[v][x],  lse[r] = log sum_v exp z[r][v],
  *   loss[r] = lse[r] - z[r][label[r]].
+ * A loss of finite logits is never below 0, and off by parts of itself and some
+ * 2^-23 whatever the logits' size.
  * A row whose label lies outside [0, V) has no target: its loss is 0 (lse is
  * written all the same).  Entries whose logit is -infinity have probability 0; a row
  * with a NaN or +infinity among its logits has lse NaN.

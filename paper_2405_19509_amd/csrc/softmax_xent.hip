@@ -34,6 +34,10 @@ constexpr float kLog2e = 1.44269504088896341f, kLn2 = 0.693147180559945309f;
 __device__ __forceinline__ int exponent(float v) { return int(__float_as_uint(v) >> 23 & 255u) - 127; }
 constexpr int kTop = 14;  // scaled values stay below 2^15, half of fp16's largest
 
+// fp32 values from 3.396e38 on round past the largest bf16, kMostBf16.  The first of three parts is therefore that of
+// kBelow times the value, which is at most kMostBf16; the other two hold the rest as well (1.5 * 2^-26 of it is left).
+constexpr float kMostBf16 = 0x1.fep127f, kBelow = 0x1.fep-1f;
+
 typedef __bf16 v4bf __attribute__((ext_vector_type(4)));
 typedef _Float16 v4hf __attribute__((ext_vector_type(4)));
 
@@ -97,7 +101,7 @@ __global__ __launch_bounds__(256) void lay_out_kernel(const T *src, int64_t rows
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
         if (NP == 2 && p == 0) v[e] = ldexpf(v[e], k);
-        w[e] = static_cast<Part<NP>>(v[e]);
+        w[e] = static_cast<Part<NP>>(NP == 3 && p == 0 ? v[e] * kBelow : v[e]);
         v[e] -= static_cast<float>(w[e]);
       }
       *reinterpret_cast<Out *>(out + (p * rows + r) * dp + c) = w;
@@ -335,6 +339,11 @@ struct Probabilities {
   float *rest; // bf16: what rounding leaves of each row's target [rows]
 };
 
+// a finite value up to the largest bf16
+__device__ __forceinline__ float within_bf16(float v) {
+  return fabsf(v) < INFINITY ? __builtin_amdgcn_fmed3f(v, -kMostBf16, kMostBf16) : v;
+}
+
 template <class P, int FB>
 __global__ __launch_bounds__(P::Threads) void p_kernel(Logits a, Probabilities b, uint32_t nf, uint32_t ns) {
   __shared__ __align__(1024) char lds[P::Lds];
@@ -399,8 +408,16 @@ __global__ __launch_bounds__(P::Threads) void p_kernel(Logits a, Probabilities b
         for (int f = 0; f < P::FT; ++f)
 #pragma unroll
           for (int i = 0; i < 16; ++i)
-            if (y == 32 * f + tile_f(i))
-              b.rest[s0 + 32 * s + li] = acc[f][s][i] - static_cast<float>(static_cast<__bf16>(acc[f][s][i]));
+            if (y == 32 * f + tile_f(i)) {
+              const float v = acc[f][s][i];
+              b.rest[s0 + 32 * s + li] = v - static_cast<float>(static_cast<__bf16>(within_bf16(v)));
+            }
+      }
+      if (__any(fabsf(w[s]) > kMostBf16)) {  // so may P be
+#pragma unroll
+        for (int f = 0; f < P::FT; ++f)
+#pragma unroll
+          for (int i = 0; i < 16; ++i) acc[f][s][i] = within_bf16(acc[f][s][i]);
       }
     }
     store_tiles<P>(lds, b.P + to, b.ld, rows, cols, [&](int f, int s, int i) { return acc[f][s][i]; });
@@ -409,13 +426,13 @@ __global__ __launch_bounds__(P::Threads) void p_kernel(Logits a, Probabilities b
       store_tiles<P>(lds, b.Q + to, b.ld, rows, cols,
                      [&](int f, int s, int i) { return ldexpf(acc[f][s][i], -kh[s]); });
     if (b.P) {
-      auto part = [&](int f, int s, int i) {  // leaves what the part leaves
-        const float v = static_cast<float>(static_cast<__bf16>(acc[f][s][i]));
-        acc[f][s][i] -= v;
-        return v;
-      };
 #pragma unroll
-      for (int p = 0; p < 3; ++p) store_tiles<P>(lds, b.P + p * a.rows * b.ld + to, b.ld, rows, cols, part);
+      for (int p = 0; p < 3; ++p)
+        store_tiles<P>(lds, b.P + p * a.rows * b.ld + to, b.ld, rows, cols, [&](int f, int s, int i) {  // leaves what the part leaves
+          const float v = static_cast<float>(static_cast<__bf16>(p == 0 ? acc[f][s][i] * kBelow : acc[f][s][i]));
+          acc[f][s][i] -= v;
+          return v;
+        });
     }
   }
 }

@@ -341,7 +341,8 @@ __global__ __launch_bounds__(MOST) __attribute__((amdgpu_waves_per_eu(4))) void 
       }
     if constexpr (!DX) continue;
     Sums::sum(part, s, int(r & 1));
-    const float ca = -rs * (s[0] * inv), ch = -rs * rs * (s[1] * inv);
+    // rstd last: its square is past the largest float for rows of deviations below 2^-64 (eps = 0)
+    const float ca = -(s[0] * inv), ch = -(s[1] * inv);
 #pragma unroll
     for (int k = 0; k < NV; ++k) {
       xr[k].forget();
@@ -349,7 +350,7 @@ __global__ __launch_bounds__(MOST) __attribute__((amdgpu_waves_per_eu(4))) void 
 #pragma unroll
       for (int q = 0; q < U / 4; ++q) {
         const Quad g = gs[k * U / 4 + q][threadIdx.x];
-        ar[k].set(q, [&](int e) { return fmaf(ar[k][e], g[e % 4] * rs, fmaf(xr[k][e] - m, ch, ca)); });
+        ar[k].set(q, [&](int e) { return rs * fmaf(ar[k][e], g[e % 4], fmaf((xr[k][e] - m) * rs, ch, ca)); });
         __builtin_amdgcn_sched_barrier(0);
       }
       ar[k].store((dx + r * d) + c[k], left[k]);

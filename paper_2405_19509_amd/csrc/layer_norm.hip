@@ -41,6 +41,23 @@ struct Unit {
         }
     }
   }
+  // past a row's end its first value again: what is made of it there is as finite as the row's own
+  __device__ __forceinline__ void fill(int left) {
+    if (left > 0 && left < U) {
+      const uint32_t first = U == 8 ? (w[0] & 0xffffu) * 0x10001u : w[0];
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        if constexpr (U == 8) {
+          if (2 * k >= left)
+            w[k] = first;
+          else if (2 * k + 1 == left)
+            w[k] |= first << 16;
+        } else {
+          if (k >= left) w[k] = first;
+        }
+      }
+    }
+  }
   __device__ __forceinline__ float operator[](int e) const {
     if constexpr (U == 8)
       return __uint_as_float(e % 2 ? w[e / 2] & 0xffff0000u : w[e / 2] << 16);
@@ -324,7 +341,9 @@ __global__ __launch_bounds__(MOST) __attribute__((amdgpu_waves_per_eu(4))) void 
     if (kAhead && r + 1 < r1) load(r + 1);
     float s[2] = {0.f, 0.f};
 #pragma unroll
-    for (int k = 0; k < NV; ++k)
+    for (int k = 0; k < NV; ++k) {
+      xr[k].fill(left[k]);
+      float ah = 0.f;
 #pragma unroll
       for (int q = 0; q < U / 4; ++q) {
         const Quad g = gs[k * U / 4 + q][threadIdx.x];
@@ -335,10 +354,12 @@ __global__ __launch_bounds__(MOST) __attribute__((amdgpu_waves_per_eu(4))) void 
           sg[k][e] += v * h;
           sb[k][e] += v;
           s[0] += a;
-          s[1] += a * h;
+          ah += a * h;
         }
         __builtin_amdgcn_sched_barrier(0);
       }
+      s[1] += left[k] > 0 ? ah : 0.f;  // of a unit past the row h, of no value of it, may be infinite
+    }
     if constexpr (!DX) continue;
     Sums::sum(part, s, int(r & 1));
     // rstd last: its square is past the largest float for rows of deviations below 2^-64 (eps = 0)
@@ -415,6 +436,7 @@ __global__ __launch_bounds__(kLongThreads) void norm_dx_long_kernel(const T *x, 
       for (int e = 0; e < U; ++e) g[e] = 1.f;
       v.load((x + r * d) + c, n);
       a.load((dy + r * d) + c, n);
+      v.fill(n);
       if (gamma) load_floats(gamma + c, n, g);
 #pragma unroll
       for (int e = 0; e < U; ++e) {  // past the row dy is zero

@@ -31,3 +31,25 @@ def test_rows_of_tiny_deviations_without_eps(d, dtype):
         b = bar[k] + more[k] + (2.0 ** -8 * ref[k].abs() * 1.01 if dtype == torch.bfloat16 and k in ("y", "dx") else 0.0)
         off = (v.double() - ref[k]).abs()
         assert bool((off <= b).all()), (k, float((off / b).max()))
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("level", [2.0 ** 108, -2.0 ** 108])
+@pytest.mark.parametrize("d", WIDTHS + [1, 2, 7, 513, 2051, 8196, 32765])
+def test_constant_rows_far_off_zero(d, level, dtype):
+    """Every sum of a row of 2^108 is exact, so h = 0 and dx = rstd (a - mean a) to the roundings of sums of d terms; what
+    a kernel makes of the places past a row's end (of zeros there: h = -2^128) is not among them."""
+    _, dy, gamma, beta = problem(2, 5, d, dtype)
+    x = torch.full_like(dy, level)
+    x[1, 1:3] = 0.0
+    got = everything(x, dy, gamma, beta, eps=2.0 ** -40)
+    assert torch.equal(got["mean"].double(), x[..., 0].double()) and bool((got["rstd"] == 2.0 ** 20).all())
+    assert torch.equal(got["y"], beta.to(dtype).expand_as(x)) and not got["dgamma"].any()
+    a = dy.double() * gamma.double()
+    want = 2.0 ** 20 * (a - a.mean(-1, keepdim=True))
+    bar = 2.0 ** 20 * (2 * d ** 0.5 + 8) * 2.0 ** -24 * (a.abs() + a.abs().mean(-1, keepdim=True))
+    if dtype == torch.bfloat16:
+        bar = bar + 2.0 ** -8 * (want.abs() + bar)
+    assert bool(((got["dx"].double() - want).abs() <= bar).all())
+    n = dy.shape[1]
+    assert bool(((got["dbeta"].double() - dy.double().sum(1)).abs() <= (2 * n ** 0.5 + 8) * 2.0 ** -24 * dy.double().abs().sum(1)).all())

@@ -293,10 +293,12 @@ __global__ __launch_bounds__(kLongThreads) void norm_long_kernel(const T *x, con
 // where a chunk is one run.
 template <typename T, int MOST, int NV, bool DX>
 __global__ __launch_bounds__(MOST) __attribute__((amdgpu_waves_per_eu(4))) void norm_grads_kernel(const T *x, const T *dy, const float *gamma, const float *mean,
-                                                             const float *rstd, int64_t n, int64_t d, int runs, int64_t per,
+                                                             const float *rstd, int N, int64_t n, int64_t d, int runs, int64_t per,
                                                              T *dx, float *sums, float *dgamma, float *dbeta) {
   constexpr int U = kUnit<T>;
-  const int64_t i = blockIdx.x / runs, run = blockIdx.x % runs;
+  const uint32_t block = block_number();
+  const int64_t i = block / runs, run = block % runs;
+  if (i >= N) return;  // the whole block
   const int64_t r0 = i * n + run * per, r1 = run * per + per < n ? r0 + per : (i + 1) * n;
   const float inv = 1.f / float(d);
   // gamma in LDS, a thread's own: sixteen registers less let rows of 16384 bf16 be loaded a row ahead
@@ -378,8 +380,8 @@ __global__ __launch_bounds__(MOST) __attribute__((amdgpu_waves_per_eu(4))) void 
       __builtin_amdgcn_sched_barrier(0);
     }
   }
-  float *og = runs > 1 ? sums + int64_t(blockIdx.x) * 2 * d : (dgamma ? dgamma + i * d : nullptr);
-  float *ob = runs > 1 ? sums + (int64_t(blockIdx.x) * 2 + 1) * d : (dbeta ? dbeta + i * d : nullptr);
+  float *og = runs > 1 ? sums + int64_t(block) * 2 * d : (dgamma ? dgamma + i * d : nullptr);
+  float *ob = runs > 1 ? sums + (int64_t(block) * 2 + 1) * d : (dbeta ? dbeta + i * d : nullptr);
 #pragma unroll
   for (int k = 0; k < NV; ++k) {
     if (og && dgamma) store_floats(og + c[k], left[k], sg[k]);
@@ -585,8 +587,8 @@ int launch_grads(const void *x, const void *dy, const float *gamma, const float 
                          dyt, gamma, mean, rstd, rows, d, dxt);
   } else {
     const int threads = threads_for<T>(units), each = units_each<T>(units);
-    GCX_ROWS(threads, each, hipLaunchKernelGGL((dx ? norm_grads_kernel<T, MOST, NV, true> : norm_grads_kernel<T, MOST, NV, false>), dim3(unsigned(N) * unsigned(runs)),
-                                     dim3(unsigned(threads)), 0, st, xt, dyt, gamma, mean, rstd, n, d, runs, per, dxt, sums, dgamma, dbeta))
+    GCX_ROWS(threads, each, hipLaunchKernelGGL((dx ? norm_grads_kernel<T, MOST, NV, true> : norm_grads_kernel<T, MOST, NV, false>), blocks_of(int64_t(N) * runs),
+                                     dim3(unsigned(threads)), 0, st, xt, dyt, gamma, mean, rstd, N, n, d, runs, per, dxt, sums, dgamma, dbeta))
   }
   if (runs > 1 && (dgamma || dbeta)) {
     auto join = [&](auto kernel, int columns, int threads) {

@@ -55,9 +55,9 @@ __global__ __launch_bounds__(256) void lay_out_kernel(const T *src, int64_t rows
                                                       unsigned *clear, int64_t count) {
   typedef T Four __attribute__((ext_vector_type(4), aligned(sizeof(T))));  // rows start anywhere
   typedef Part<NP> Out __attribute__((ext_vector_type(4)));
-  for (int64_t e = int64_t(blockIdx.x) * 256 + threadIdx.x; e < count; e += int64_t(gridDim.x) * 256) clear[e] = 0;
+  for (int64_t e = int64_t(block_number()) * 256 + threadIdx.x; e < count; e += int64_t(gridDim.x) * gridDim.y * 256) clear[e] = 0;
   const int lane = threadIdx.x % kWave;
-  const int64_t r = int64_t(blockIdx.x) * 4 + threadIdx.x / kWave;
+  const int64_t r = int64_t(block_number()) * 4 + threadIdx.x / kWave;
   if (r >= rows) return;
   const T *row = src + r * d;
   bool zero = false;
@@ -222,7 +222,7 @@ __global__ __launch_bounds__(P::Threads) void lse_part_kernel(Logits a, uint32_t
   float *own = reinterpret_cast<float *>(red + P::WF * P::TS);  // [TS]: the targets' logits, where loss is given
   Pipe<P, true, true, FB> pipe(lds);
   int ft, st;
-  if (!tile_of(blockIdx.x, nf, ns, ft, st)) return;
+  if (!tile_of(block_number(), nf, ns, ft, st)) return;
   pipe.start(a.W.along(int64_t(ft) * P::TF, a.width, 0), a.H.along(int64_t(st) * P::TS, a.rows, 0), a.K);
   const int64_t f0 = int64_t(ft) * P::TF + wf * P::FT * 32, s0 = int64_t(st) * P::TS + ws * P::ST * 32;
   int32_t label[P::ST];
@@ -300,7 +300,7 @@ __global__ __launch_bounds__(256) void lse_join_kernel(const float2 *part, const
   constexpr int kEach = 256 / kJoin;
   __shared__ float2 red[kEach][kJoin];
   const int c = threadIdx.x % kJoin, g = threadIdx.x / kJoin;
-  const int64_t r = int64_t(blockIdx.x) * kJoin + c;
+  const int64_t r = int64_t(block_number()) * kJoin + c;
   float m = -INFINITY, sum = 0.f;
   if (r < rows) {
 #pragma unroll 4
@@ -351,7 +351,7 @@ __global__ __launch_bounds__(P::Threads) void p_kernel(Logits a, Probabilities b
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), wf = wave % P::WF, ws = wave / P::WF;
   Pipe<P, true, true, FB> pipe(lds);
   int ft, st;
-  if (!tile_of(blockIdx.x, nf, ns, ft, st)) return;
+  if (!tile_of(block_number(), nf, ns, ft, st)) return;
   pipe.start(a.W.along(int64_t(ft) * P::TF, a.width, 0), a.H.along(int64_t(st) * P::TS, a.rows, 0), a.K);
   const int64_t f0 = int64_t(ft) * P::TF + wf * P::FT * 32, s0 = int64_t(st) * P::TS + ws * P::ST * 32;
   int32_t label[P::ST];
@@ -520,8 +520,8 @@ __global__ __launch_bounds__(P::Threads) void dh_kernel(Matrix Pm, Matrix W, int
                                                         const int32_t *label, int32_t V, const float *rest) {
   __shared__ __align__(1024) char lds[P::Lds];
   int ft, st;
-  if (!tile_of(blockIdx.x, nf, ns * together, ft, st)) return;
-  const int64_t split = int64_t(blockIdx.y) * together + st / int(ns);
+  if (!tile_of(block_number(), nf, ns * together, ft, st)) return;
+  const int64_t split = int64_t(blockIdx.z) * together + st / int(ns);
   st %= int(ns);
   const int lane = threadIdx.x % kWave, h = lane >> 5, li = lane & 31;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), wf = wave % P::WF, ws = wave / P::WF;
@@ -696,7 +696,7 @@ __global__ __launch_bounds__(P::Threads) void g_kernel(Matrix Pm, Matrix H, int6
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), wf = wave % P::WF, ws = wave / P::WF;
   Pipe<P, false, false> pipe(lds);
   int ft, st;
-  if (!tile_of(blockIdx.x, nf, ns * N, ft, st)) return;
+  if (!tile_of(block_number(), nf, ns * N, ft, st)) return;
   const int64_t i = st / int(ns), c = st % int(ns);
   pipe.start(H.across(int64_t(ft) * P::TF, i * n, (i + 1) * n), Pm.across(c * P::TS, i * n, (i + 1) * n), n);
   const int64_t f0 = int64_t(ft) * P::TF + wf * P::FT * 32, s0 = c * P::TS + ws * P::ST * 32;
@@ -736,8 +736,10 @@ __global__ __launch_bounds__(256) void g_few_kernel(const char *Pm, int64_t ld, 
   typedef uint32_t Words __attribute__((ext_vector_type(4)));
   typedef uint32_t Anywhere __attribute__((ext_vector_type(4), aligned(2)));
   __shared__ __align__(16) float p[kFewEntries][MOST + (MOST > 4 ? 4 : 0)];  // neighbours' writes to other banks
-  const int64_t i = blockIdx.x / nx / nv, first = int64_t(blockIdx.x / nx % nv) * entries;
-  const int64_t x = (int64_t(blockIdx.x % nx) * tx + threadIdx.x % tx) * U;
+  const uint32_t block = block_number();
+  const int64_t i = block / nx / nv, first = int64_t(block / nx % nv) * entries;
+  if (i * n >= rows) return;  // the whole block
+  const int64_t x = (int64_t(block % nx) * tx + threadIdx.x % tx) * U;
   const int here = width - first < entries ? int(width - first) : entries;
   for (int e = threadIdx.x; e < MOST * entries; e += 256) {
     const int t = e / entries, v = e % entries;
@@ -882,7 +884,7 @@ Tiling tiling(int64_t w, int64_t rows, int64_t K, int NP) {
 // 1665 / 1838, 24810 x 484 219 / 273; 200 rows 2236 / 1942 and 292 / 246; 200 rows, 8192 x 1000 176 / 201)
 bool direct_pays(int64_t rows, int64_t V, int64_t d) { return rows <= 160 || rows * V * d <= int64_t(1) << 27; }
 
-unsigned grid(int64_t total) { return unsigned(up(total, 8)); }
+dim3 grid(int64_t total) { return blocks_of(up(total, 8)); }
 
 // One workspace, cut into pieces of whole 256 bytes; with base NULL only the size.
 struct Cut {
@@ -972,13 +974,17 @@ Plan plan(int64_t N, int64_t n, int64_t V, int64_t d, int32_t dtype, bool grads,
   return p;
 }
 
+// Tiles are numbered in 32 bits.  The kernels over P's columns take one row of the grid, past which P does not fit a
+// device.
 bool xent_sizes_ok(int64_t rows, int64_t N, int64_t V, int64_t d, int32_t dtype) {
   return rows >= 0 && N >= 0 && V >= 1 && d >= 1 && d <= int64_t(1) << 20 && (dtype == GC_F32 || dtype == GC_BF16) &&
          rows <= int64_t(1) << 31 && sizes_ok({rows, d}) && sizes_ok({rows, V}) && sizes_ok({N, V, d}) &&
-         // blocks of the smallest tiles
+         // the smallest tiles
          sizes_ok({ceil_div(rows, 32), ceil_div(V, 128)}) && ceil_div(rows, 32) * ceil_div(V, 128) < int64_t(1) << 30 &&
+         ceil_div(rows, 32) * ceil_div(d, 128) < int64_t(1) << 30 &&
          N * ceil_div(d, 128) * ceil_div(std::min(V, piece(rows, V, up(d, 8))), 32) < int64_t(1) << 30 &&
-         (rows + N) * (piece(rows, V, up(d, 8)) / 64) < int64_t(1) << 30;
+         (dtype == GC_BF16 || direct_pays(rows, V, d) || rows <= kFewRows<float> * N ||
+          grid_ok(N * (piece(rows, V, up(d, 8)) / 64) * ceil_div(rows / N, kColumnRows), 256));
 }
 
 #define GCX_SHAPE(size, NP, ...)           \
@@ -1005,7 +1011,7 @@ template <typename T, int NP>
 void lay_out(const void *src, int64_t first, int64_t rows, int64_t d, int64_t dp, const int32_t *label, int32_t V, void *out,
              int *exps, hipStream_t st, unsigned *clear = nullptr, int64_t count = 0) {
   const T *s = static_cast<const T *>(src) + first * d;
-  hipLaunchKernelGGL((lay_out_kernel<T, NP>), dim3(unsigned(ceil_div(rows, 4))), dim3(256), 0, st, s, rows, d, dp,
+  hipLaunchKernelGGL((lay_out_kernel<T, NP>), blocks_of(ceil_div(rows, 4)), dim3(256), 0, st, s, rows, d, dp,
                      label, V, static_cast<Part<NP> *>(out), exps, clear, count);
 }
 
@@ -1055,7 +1061,7 @@ int launch_xent(const Plan &p, const void *H, const void *W, const int32_t *labe
     auto launch = [&](const Logits &a, Size size) {
       const int64_t total = tiles(size, a.width, p.rows, 1, nf, ns);
       by_alignment<NP, T>(W, p.d, [&](auto fb) {
-        GCX_SHAPE(size, NP, hipLaunchKernelGGL((lse_part_kernel<P, decltype(fb)::value>), dim3(grid(total)), dim3(P::Threads), 0, st, a,
+        GCX_SHAPE(size, NP, hipLaunchKernelGGL((lse_part_kernel<P, decltype(fb)::value>), grid(total), dim3(P::Threads), 0, st, a,
                                                nf, ns, tile0, p.part, p.target, int32_t(p.V), at_once ? loss : nullptr, lse))
       });
       tile0 += nf;
@@ -1064,7 +1070,7 @@ int launch_xent(const Plan &p, const void *H, const void *W, const int32_t *labe
     if (t.first < w) launch(whole.part(t.first, w), t.then);
   }
   if (!at_once)
-    hipLaunchKernelGGL(lse_join_kernel, dim3(unsigned(ceil_div(p.rows, kJoin))), dim3(256), 0, st, p.part, p.target, label,
+    hipLaunchKernelGGL(lse_join_kernel, blocks_of(ceil_div(p.rows, kJoin)), dim3(256), 0, st, p.part, p.target, label,
                        p.rows, int32_t(p.V), tile0, loss, lse);
   return launch_status();
 }
@@ -1099,7 +1105,7 @@ int launch_xent_grads(const Plan &p, const void *H, const void *W, const int32_t
         const Logits a = whole.part(from, to);
         const Probabilities b{lse, dloss, int32_t(p.V), p.ld, p.ld - from, Pb ? Pb + from : nullptr, Q ? Q + from : nullptr, p.rest};
         by_alignment<NP, T>(W, p.d, [&](auto fb) {
-          GCX_SHAPE(size, NP, hipLaunchKernelGGL((p_kernel<P, decltype(fb)::value>), dim3(grid(total)), dim3(P::Threads), 0, st, a, b, nf, ns))
+          GCX_SHAPE(size, NP, hipLaunchKernelGGL((p_kernel<P, decltype(fb)::value>), grid(total), dim3(P::Threads), 0, st, a, b, nf, ns))
         });
       };
       launch(0, t.first, t.size);
@@ -1116,10 +1122,12 @@ int launch_xent_grads(const Plan &p, const void *H, const void *W, const int32_t
       // ones (8 rows, 65536 x 216 fp32: 42 us, so 14).  Others do better a split at a time (4096 x 65536 x 2048 bf16: 45
       // of 3870 us; 12 rows, 65536 x 4096 fp32: 574 / 605).
       const int64_t splits = ceil_div(w, p.kper), one = tiles(p.dh_size, p.d, p.rows, 1, nf, ns);
-      const int64_t together = grid(one) * 4 > one * 5 ? splits : 1, total = one * together;
+      const int64_t together = up(one, 8) * 4 > one * 5 ? splits : 1, total = one * together;
+      dim3 blocks = grid(total);
+      blocks.z = unsigned(splits / together);
       by_alignment<NP, T>(W, p.d, [&](auto fb) {
         GCX_SHAPE(p.dh_size, NPh,
-                  hipLaunchKernelGGL((dh_kernel<P, T, decltype(fb)::value>), dim3(grid(total), unsigned(splits / together)), dim3(P::Threads), 0, st, Pm, Wh,
+                  hipLaunchKernelGGL((dh_kernel<P, T, decltype(fb)::value>), blocks, dim3(P::Threads), 0, st, Pm, Wh,
                                      p.rows, w, p.d, p.dq, p.kper, v0 == 0, nf, ns, uint32_t(together), p.sum,
                                      at_once ? static_cast<T *>(dH) : nullptr, label, int32_t(p.V), p.rest))
       });
@@ -1131,7 +1139,7 @@ int launch_xent_grads(const Plan &p, const void *H, const void *W, const int32_t
       const int entries = std::min(kFewEntries, 256 / tx * 32);
       const unsigned nx = unsigned(ceil_div(units, tx)), nv = unsigned(ceil_div(w, entries));
       auto few = [&](auto kernel) {
-        hipLaunchKernelGGL(kernel, dim3(nx * nv * unsigned(p.N)), dim3(256), 0, st, NP == 1 ? p.P : reinterpret_cast<char *>(p.Q),
+        hipLaunchKernelGGL(kernel, blocks_of(int64_t(nx) * nv * p.N), dim3(256), 0, st, NP == 1 ? p.P : reinterpret_cast<char *>(p.Q),
                            p.ld, p.H, p.dp, p.rows, int(p.n), w, p.d, p.V, v0, tx, nx, nv, entries, label, p.rest,
                            static_cast<T *>(G));
       };
@@ -1145,7 +1153,7 @@ int launch_xent_grads(const Plan &p, const void *H, const void *W, const int32_t
       }
       const Size size = size_for(p.d, w, p.N, p.n, NP);
       const int64_t total = tiles(size, p.d, w, p.N, nf, ns);
-      GCX_SHAPE(size, NP, hipLaunchKernelGGL((g_kernel<P, T>), dim3(grid(total)), dim3(P::Threads), 0, st, Gm, Hm, p.n, w, p.ld,
+      GCX_SHAPE(size, NP, hipLaunchKernelGGL((g_kernel<P, T>), grid(total), dim3(P::Threads), 0, st, Gm, Hm, p.n, w, p.ld,
                                              p.d, p.dp, p.V, v0, nf, ns, p.N, p.top, label, p.rest, static_cast<T *>(G)))
     }
   }

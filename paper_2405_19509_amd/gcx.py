@@ -144,6 +144,13 @@ def _dev(t, name, dtype, shape=None):
     return t.data_ptr()
 
 
+def _fits(*sizes):
+    """Sizes that a call takes as 32-bit integers, into which ctypes would cut larger ones silently."""
+    for v in sizes:
+        if not -(1 << 31) <= v < 1 << 31:
+            raise ValueError(f"a size of {v} does not fit 32 bits")
+
+
 def _g_dtype(G):
     torch = _torch()
     if G.dtype == torch.float32:
@@ -449,14 +456,15 @@ def _chunks(t, name):
     """(N, n, d) of a tensor [N][n][d]."""
     if t.dim() != 3:
         raise ValueError(f"{name} must be [N][n][d]")
-    return t.shape
+    N, n, d = t.shape
+    _fits(N, n)
+    return N, n, d
 
 
 def _vocabulary(W):
-    """V of W [V][d], which has to fit the calls' 32 bits."""
+    """V of W [V][d]."""
     V = W.shape[0]
-    if V >= 1 << 31:
-        raise ValueError("W has 2^31 rows or more")
+    _fits(V)
     return V
 
 
@@ -537,6 +545,7 @@ def gc_layer_norm(x, gamma=None, beta=None, eps: float = 1e-5, y=None, mean=None
 
 
 def gc_layer_norm_grads_workspace_size(N: int, n: int, d: int) -> int:
+    _fits(N, n)
     return int(load().gc_layer_norm_grads_workspace_size(N, n, d))
 
 
@@ -562,6 +571,7 @@ def gc_layer_norm_grads(x, dy, gamma, mean, rstd, dx=None, dgamma=None, dbeta=No
 
 
 def gc_softmax_xent_workspace_size(rows: int, V: int, d: int, dtype: int) -> int:
+    _fits(V)
     return int(load().gc_softmax_xent_workspace_size(rows, V, d, dtype))
 
 
@@ -582,6 +592,7 @@ def gc_softmax_xent(H, W, label, loss=None, lse=None, workspace=None, stream=Non
 
 
 def gc_softmax_xent_grads_workspace_size(N: int, n: int, V: int, d: int, dtype: int) -> int:
+    _fits(N, n, V)
     return int(load().gc_softmax_xent_grads_workspace_size(N, n, V, d, dtype))
 
 

@@ -37,3 +37,27 @@ def test_gradients(N, n, V, d, dtype, taken):
     assert (gcx.gc_softmax_xent_grads_workspace_size(N, n, V, d, dtype) > 0) == taken
     st = gcx.load().gc_softmax_xent_grads(P, P, P, P, None, N, n, V, d, dtype, P, P, P, 16, None)
     assert st == gcx.GC_EINVAL
+
+
+def test_sizes_that_do_not_fit_32_bits():
+    """2^32 + 5 is not taken for 5."""
+    torch = pytest.importorskip("torch")
+    big = 2 ** 32 + 5
+
+    def t(*shape, dtype=torch.float32):
+        return torch.empty(shape, dtype=dtype, device="meta")
+
+    i32 = torch.int32
+    for call in (lambda: gcx.gc_layer_norm_grads(t(1, big, 8), t(1, big, 8), None, t(1, big), t(1, big)),
+                 lambda: gcx.gc_layer_norm_grads(t(big, 1, 8), t(big, 1, 8), None, t(big, 1), t(big, 1)),
+                 lambda: gcx.gc_softmax_xent_grads(t(1, big, 8), t(9, 8), t(1, big, dtype=i32), t(1, big)),
+                 lambda: gcx.gc_softmax_xent_grads(t(big, 1, 8), t(9, 8), t(big, 1, dtype=i32), t(big, 1)),
+                 lambda: gcx.gc_softmax_xent_grads(t(1, 5, 8), t(big, 8), t(1, 5, dtype=i32), t(1, 5)),
+                 lambda: gcx.gc_softmax_xent(t(5, 8), t(big, 8), t(5, dtype=i32)),
+                 lambda: gcx.gc_layer_norm_grads_workspace_size(big, 5, 8), lambda: gcx.gc_layer_norm_grads_workspace_size(5, big, 8),
+                 lambda: gcx.gc_softmax_xent_workspace_size(5, big, 8, F32),
+                 lambda: gcx.gc_softmax_xent_grads_workspace_size(big, 5, 9, 8, F32),
+                 lambda: gcx.gc_softmax_xent_grads_workspace_size(5, big, 9, 8, BF16),
+                 lambda: gcx.gc_softmax_xent_grads_workspace_size(5, 5, big, 8, BF16)):
+        with pytest.raises(ValueError, match="32 bits"):
+            call()

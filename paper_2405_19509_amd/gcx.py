@@ -167,6 +167,7 @@ def gc_assign(kind: int, N: int, m: int, s: int = -1, O: Optional[np.ndarray] = 
     """Host call.  Returns (O, order, holder, hpos) as int32 numpy arrays.  For
     GC_ASSIGN_REGULAR, O is the support on input and the returned O the ordering."""
     lib = load()
+    _fits(N, m, s, delta or 0, gamma or 0)
     if kind == GC_ASSIGN_CYCLIC:
         delta = s + 1 if delta is None else delta
         gamma = s + 1 if gamma is None else gamma
@@ -192,6 +193,7 @@ def gc_qmax(O):
     """O [N][m] ordering matrix (host) -> (Q [N] int64, Q_max): the Sec. 3 metric."""
     O = np.ascontiguousarray(O, dtype=np.int32)
     N, m = O.shape
+    _fits(N, m)
     Q = np.empty(N, dtype=np.int64)
     qmax = ctypes.c_int64(0)
     _check("gc_qmax", load().gc_qmax(O.ctypes.data, N, m, Q.ctypes.data, ctypes.byref(qmax)))
@@ -199,6 +201,7 @@ def gc_qmax(O):
 
 
 def gc_chunk_grads_workspace_size(N: int, n: int, d: int, b: int) -> int:
+    _fits(N, n, b)
     return int(load().gc_chunk_grads_workspace_size(N, n, d, b))
 
 
@@ -228,6 +231,7 @@ def gc_sum_chunks(G, gsum=None, stream=None):
     """G [N][d] (fp32 or bf16) -> gsum [d] fp32."""
     torch = _torch()
     N, d = G.shape
+    _fits(N)
     if gsum is None:
         gsum = torch.empty(d, dtype=torch.float32, device=G.device)
     st = load().gc_sum_chunks(_dev(G, "G", G.dtype), _g_dtype(G), N, d,
@@ -248,6 +252,7 @@ def gc_decode_coeffs(psi, order, holder, hpos, R, cov=None, dec=None, coef_err=N
     ell = R.shape[0]
     if m2 != m or R.shape[1] != m:
         raise ValueError("psi, order and R disagree on m")
+    _fits(N, m, delta, gamma, ell)
     dv = psi.device
     if cov is None:
         cov = torch.empty((P, N), dtype=torch.int32, device=dv)
@@ -273,6 +278,7 @@ def gc_encode(G, psi, order, Bc, T=None, stream=None):
     torch = _torch()
     N, d = G.shape
     P, m, delta, ell = Bc.shape
+    _fits(N, m, delta, ell)
     L = -(-d // ell)
     if T is None:
         T = torch.empty((P, m, L), dtype=torch.float32, device=G.device)
@@ -286,6 +292,7 @@ def gc_encode(G, psi, order, Bc, T=None, stream=None):
 
 
 def gc_reconstruct_workspace_size(P: int, m: int, d: int, ell: int) -> int:
+    _fits(m, ell)
     return int(load().gc_reconstruct_workspace_size(P, m, d, ell))
 
 
@@ -296,6 +303,7 @@ def gc_reconstruct(T, R, d: int, psi, ghat=None, gsum=None, sqerr=None, want_gha
     torch = _torch()
     P, m, L = T.shape
     ell = R.shape[0]
+    _fits(m, ell)
     if L != -(-d // ell):
         raise ValueError("T's row length does not match ceil(d / ell)")
     dv = T.device
@@ -328,6 +336,7 @@ def gc_reconstruct_noalloc(T, R, d: int, psi, ghat, gsum=None, sqerr=None, strea
     torch = _torch()
     P, m, L = T.shape
     ell = R.shape[0]
+    _fits(m, ell)
     if L != -(-d // ell):
         raise ValueError("T's row length does not match ceil(d / ell)")
     st = load().gc_reconstruct_noalloc(
@@ -341,6 +350,7 @@ def gc_reconstruct_noalloc(T, R, d: int, psi, ghat, gsum=None, sqerr=None, strea
 
 
 def gc_decode_direct_workspace_size(P: int, N: int, d: int, ell: int) -> int:
+    _fits(N, ell)
     return int(load().gc_decode_direct_workspace_size(P, N, d, ell))
 
 
@@ -355,6 +365,7 @@ def gc_decode_direct(G, psi, order, holder, hpos, R, ghat=None, gsum=None, sqerr
     ell = R.shape[0]
     delta = order.shape[1]
     gamma = holder.shape[1]
+    _fits(N, m, delta, gamma, ell)
     dv = G.device
     if want_ghat and ghat is None:
         ghat = torch.empty((P, d), dtype=torch.float32, device=dv)
@@ -380,6 +391,7 @@ def gc_progress(tau, T, failed=None, psi=None, stream=None):
     torch = _torch()
     R, m, delta = tau.shape
     G = T.shape[0]
+    _fits(m, delta, G)
     if psi is None:
         psi = torch.empty((R, G, m), dtype=torch.int32, device=tau.device)
     st = load().gc_progress(_dev(tau, "tau", torch.float64),
@@ -396,6 +408,7 @@ def gc_completion_times(tau, holder, hpos, ell: int, failed=None, partial=None, 
     torch = _torch()
     R, m, delta = tau.shape
     N, gamma = holder.shape
+    _fits(N, m, delta, gamma, ell)
     if partial is None:
         partial = torch.empty(R, dtype=torch.float64, device=tau.device)
     if original is None:
@@ -418,6 +431,7 @@ def gc_original_ls(psi, order, holder, max_iter: int = 1000, tol: float = 1e-12,
     P, m = psi.shape
     _, delta = order.shape
     N, gamma = holder.shape
+    _fits(N, m, delta, gamma, max_iter)
     if err is None:
         err = torch.empty(P, dtype=torch.float64, device=psi.device)
     if iters is None:

@@ -365,7 +365,8 @@ int gc_dropout(const void *x, const void *addend, int64_t rows, int64_t d, doubl
  *   y = (x - mean) rstd gamma + beta.
  * x, y [rows][d] device in dtype (GC_F32 or GC_BF16); gamma, beta [d] device fp32,
  * either may be NULL (ones, zeros); mean, rstd [rows] device fp32, which the
- * gradients take.  Sums of fp32; the variance from the differences to the mean.
+ * gradients take.  Sums of fp32, which a row's sum and the squares of its deviations
+ * have to fit; the variance from the differences to the mean.
  * eps >= 0.  y may be x.  rows = 0 is a no-op.
  */
 int gc_layer_norm(const void *x, const float *gamma, const float *beta, int64_t rows, int64_t d, double eps,
@@ -404,8 +405,9 @@ int gc_layer_norm_grads(const void *x, const void *dy, const float *gamma, const
  * rows = 0 is a no-op.  The sums' order is fixed by the sizes.
  * workspace: device, 16-byte aligned, at least
  * gc_softmax_xent_workspace_size(rows, V, d, dtype) bytes.
- * Errors: GC_EINVAL for sizes < 1 (rows < 0), d > 2^20, a null pointer, an unknown dtype, or
- * a workspace that is too small or unaligned.
+ * Errors: GC_EINVAL for sizes < 1 (rows < 0), d > 2^20, more than 2^31 rows or 2^30 tiles
+ * of 32 rows and 128 entries, a null pointer, an unknown dtype, or a workspace that is
+ * too small or unaligned.
  */
 size_t gc_softmax_xent_workspace_size(int64_t rows, int32_t V, int64_t d, int32_t dtype);
 int gc_softmax_xent(const void *H, const void *W, const int32_t *label, int64_t rows, int32_t V, int64_t d,
